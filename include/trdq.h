@@ -586,7 +586,7 @@ trdq_status trdq_block_norm(const trdq_norm *n, const void *X_dev, int64_t ldx, 
 /* trdq_block_norm_bwd: gradients of the above.  Xout: the stream as the norm read it (X without a branch); Y as there (or NULL);
  * dXout (stream's type, NULL = 0) and dH (bf16): what arrives at x' and h; dX (stream's type, may be dXout) and dY (bf16, with Y;
  * may be Y): what leaves.  Statistics are computed again.  Gradients of parameters, float32 and dense: dscale, dshift [segments, c], dgate
- * [segments, c] or [c], the others [c]; each may be NULL, and is if its parameter is.  Written, not added to; sums over rows run in a
+ * [segments, c], or [c] of a gate with ld_gate == 0, the others [c]; each may be NULL, and is if its parameter is.  Written, not added to; sums over rows run in a
  * fixed order.  ws_dev: trdq_block_norm_bwd_ws_nbytes(rows, c, segments) bytes, 16-byte aligned, the call's own until it has
  * finished (may be NULL if no parameter's gradient is asked for).  rows == 0 writes zeros to nothing: a no-op.
  * Errors as trdq_block_norm; a parameter's gradient without the parameter -> ERR_NULL; Y without dY or dY without Y, a workspace that

@@ -298,6 +298,9 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         g.dscale_dev = gradient(a[6], segments, d.c, "dscale");
         g.dshift_dev = gradient(a[7], segments, d.c, "dshift");
         g.dgate_dev = gradient(a[8], gate && gate->dim() == 2 ? segments : -1, d.c, "dgate");
+        // (an expanded vector: the library would take its gradient for a vector's too, and leave the other segments' unwritten)
+        if (g.dgate_dev && gate && gate->dim() == 2 && d.rows > 0 && segments > 1 && d.ld_gate == 0)
+            throw Bad{TRDQ_ERR_SHAPE, "dgate: the gate is one vector for every segment; give it and its gradient as vectors"};
         g.dpre_weight_dev = gradient(a[9], -1, d.c, "dpre_weight");
         g.dpre_bias_dev = gradient(a[10], -1, d.c, "dpre_bias");
         g.dpost_weight_dev = gradient(a[11], -1, d.c, "dpost_weight");

@@ -1,0 +1,37 @@
+"""Calls around a block's linears at the edges of what they accept, without a GPU: what is refused, and sizes that the library computes on
+the host.  (Without a device a call whose arguments are right ends in ERR_HIP: nothing can be launched.)"""
+import pytest
+import torch
+
+from paper_2503_06564_amd import trdq
+
+X = torch.zeros(6, 40, dtype=torch.bfloat16)
+WS = torch.zeros(1 << 20, dtype=torch.uint8)
+
+
+def status(f, *args, **kw):
+    """The status of a call whose tensors lie on the host; never run where a device could be handed their addresses."""
+    with pytest.raises(trdq.TrdqError) as e:
+        f(*args, stream=0, **kw)
+    return e.value.status
+
+
+def accepted():
+    """What a call with right arguments answers here: host tensors are refused where there is a device."""
+    return trdq.ERR_MISMATCH if torch.cuda.is_available() else trdq.ERR_HIP
+
+
+def test_gate_of_one_row_has_no_gradient_per_segment():
+    """An expanded vector reads as a gate, but [segments, c] cannot be its gradient: the library takes a gate without a row stride for
+    one vector."""
+    gate, kw = torch.ones(40).expand(3, 40), dict(Y=X, seg_len=2, ws=WS)
+    for d in (torch.zeros(3, 40), torch.zeros(40)):
+        assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate, dgate=d, **kw) == trdq.ERR_SHAPE
+    off = torch.tensor([0, 1, 4, 6], dtype=torch.int32)
+    assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate, dgate=torch.zeros(3, 40), Y=X, seg_off=off, ws=WS) == trdq.ERR_SHAPE
+    # the gate itself, its gradient not asked for, a vector's and a matrix' own gradients: as before
+    assert status(trdq.block_norm, X, X, X, Y=X, gate=gate, seg_len=2) == accepted()
+    assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate, **kw) == accepted()
+    assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate[0], dgate=torch.zeros(40), **kw) == accepted()
+    assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate.contiguous(), dgate=torch.zeros(3, 40), **kw) == accepted()
+    assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate[:1], dgate=torch.zeros(1, 40), Y=X, ws=WS) == accepted()
