@@ -588,7 +588,8 @@ trdq_status trdq_block_norm(const trdq_norm *n, const void *X_dev, int64_t ldx, 
  * may be Y): what leaves.  Statistics are computed again.  Gradients of parameters, float32 and dense: dscale, dshift [segments, c], dgate
  * [segments, c], or [c] of a gate with ld_gate == 0, the others [c]; each may be NULL, and is if its parameter is.  Written, not added to; sums over rows run in a
  * fixed order.  ws_dev: trdq_block_norm_bwd_ws_nbytes(rows, c, segments) bytes, 16-byte aligned, the call's own until it has
- * finished (may be NULL if no parameter's gradient is asked for).  rows == 0 writes zeros to nothing: a no-op.
+ * finished (may be NULL if no parameter's gradient is asked for).  rows == 0: the gradients asked for become zeros, nothing else
+ * is read or written (dscale, dshift and a dgate by segment have no rows then with seg_len > 0, n_seg rows with seg_off).
  * Errors as trdq_block_norm; a parameter's gradient without the parameter -> ERR_NULL; Y without dY or dY without Y, a workspace that
  * is too small -> ERR_SHAPE. */
 typedef struct trdq_norm_grads {

@@ -172,25 +172,33 @@ trdq_status trdq_block_norm_bwd(const trdq_norm *n, const trdq_norm_grads *g, vo
     int64_t segments = 0;
     TRDQ_TRY(check_norm(n, &segments));
     if (!g) return TRDQ_ERR_NULL;
-    if (n->rows == 0) return TRDQ_OK;
-    const size_t xs = size_of(n->x_dtype);
-    TRDQ_TRY(check_matrix(g->Xout_dev, n->rows, n->c, g->ldxo, xs));
-    TRDQ_TRY(check_matrix(g->dH_dev, n->rows, n->c, g->lddh, 2));
-    TRDQ_TRY(check_matrix(g->dX_dev, n->rows, n->c, g->lddx, xs));
-    if (g->dXout_dev) TRDQ_TRY(check_matrix(g->dXout_dev, n->rows, n->c, g->lddxo, xs));
-    if (!g->Y_dev != !g->dY_dev) return TRDQ_ERR_SHAPE;
-    if (g->Y_dev) {
-        TRDQ_TRY(check_matrix(g->Y_dev, n->rows, n->c, g->ldy, 2));
-        TRDQ_TRY(check_matrix(g->dY_dev, n->rows, n->c, g->lddy, 2));
+    const bool none = n->rows == 0;                    // no row to read or write, but parameters' gradients, which are zeros
+    if (!none) {
+        const size_t xs = size_of(n->x_dtype);
+        TRDQ_TRY(check_matrix(g->Xout_dev, n->rows, n->c, g->ldxo, xs));
+        TRDQ_TRY(check_matrix(g->dH_dev, n->rows, n->c, g->lddh, 2));
+        TRDQ_TRY(check_matrix(g->dX_dev, n->rows, n->c, g->lddx, xs));
+        if (g->dXout_dev) TRDQ_TRY(check_matrix(g->dXout_dev, n->rows, n->c, g->lddxo, xs));
+        if (!g->Y_dev != !g->dY_dev) return TRDQ_ERR_SHAPE;
+        if (g->Y_dev) {
+            TRDQ_TRY(check_matrix(g->Y_dev, n->rows, n->c, g->ldy, 2));
+            TRDQ_TRY(check_matrix(g->dY_dev, n->rows, n->c, g->lddy, 2));
+        }
     }
-    const void *const params[] = {n->scale, n->shift, g->Y_dev ? n->gate : nullptr, n->pre_weight, n->pre_bias,
-                                  g->Y_dev ? n->post_weight : nullptr, g->Y_dev ? n->post_bias : nullptr};
+    const bool branch = none || g->Y_dev;              // (a branch of no rows need not have an address)
+    const void *const params[] = {n->scale, n->shift, branch ? n->gate : nullptr, n->pre_weight, n->pre_bias,
+                                  branch ? n->post_weight : nullptr, branch ? n->post_bias : nullptr};
     float *const grads[] = {g->dscale_dev, g->dshift_dev, g->dgate_dev, g->dpre_weight_dev, g->dpre_bias_dev, g->dpost_weight_dev, g->dpost_bias_dev};
     bool any = false;
     for (int i = 0; i < 7; ++i) {
         if (grads[i] && !params[i]) return TRDQ_ERR_NULL;
         if (!aligned(grads[i], 4)) return TRDQ_ERR_SHAPE;
         any = any || grads[i];
+    }
+    if (none) {
+        const int64_t per_segment = segments * n->c, vector = n->c;
+        const int64_t sizes[] = {per_segment, per_segment, n->ld_gate != 0 ? per_segment : vector, vector, vector, vector, vector};
+        return hip_status(trdq::launch_zero_gradients(grads, sizes, static_cast<hipStream_t>(stream)));
     }
     trdq::NormArgs a = norm_args(*n, segments);
     if (any) {

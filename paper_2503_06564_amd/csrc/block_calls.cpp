@@ -229,6 +229,11 @@ trdq_norm norm_of(const at::Tensor &X, PyObject *const *a, int64_t *segments_out
             const Matrix g = matrix(gate, segments, c, "gate");
             d.gate = g.p; d.ld_gate = g.ld;
         }
+    } else {
+        // no row reads them (their segments may be those of no rows); their gradients are zeros
+        d.scale = scale ? address(*scale, "scale") : nullptr; d.ld_scale = c;
+        d.shift = shift ? address(*shift, "shift") : nullptr; d.ld_shift = c;
+        d.gate = gate ? address(*gate, "gate") : nullptr; d.ld_gate = gate && gate->dim() == 2 ? c : 0;
     }
     *segments_out = segments;
     return d;
@@ -299,7 +304,7 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         g.dshift_dev = gradient(a[7], segments, d.c, "dshift");
         g.dgate_dev = gradient(a[8], gate && gate->dim() == 2 ? segments : -1, d.c, "dgate");
         // (an expanded vector: the library would take its gradient for a vector's too, and leave the other segments' unwritten)
-        if (g.dgate_dev && gate && gate->dim() == 2 && d.rows > 0 && segments > 1 && d.ld_gate == 0)
+        if (g.dgate_dev && gate && gate->dim() == 2 && segments > 1 && d.ld_gate == 0)
             throw Bad{TRDQ_ERR_SHAPE, "dgate: the gate is one vector for every segment; give it and its gradient as vectors"};
         g.dpre_weight_dev = gradient(a[9], -1, d.c, "dpre_weight");
         g.dpre_bias_dev = gradient(a[10], -1, d.c, "dpre_bias");

@@ -595,6 +595,17 @@ __global__ __launch_bounds__(kJoinThreads) void block_norm_join_kernel(NormArgs 
     if (a.dpost_b) a.dpost_b[k] = gate * all[3];
 }
 
+// Gradients of a call without rows: sums over nothing.
+struct ZeroArgs {
+    float *to[7];
+    int64_t n[7];
+};
+__global__ __launch_bounds__(256) void block_norm_zero_kernel(ZeroArgs a)
+{
+    float *const to = a.to[blockIdx.y];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.n[blockIdx.y]; i += (int64_t)gridDim.x * 256) to[i] = 0.0f;
+}
+
 // Waves of a row and pieces of a lane.  Up to 1024 values one wave.  Up to 1536 the gradient keeps one wave (three waves a row, each with its
 // sums to write: 4096 x 1152 26 us in place of 21); forward three waves with one piece a lane take 57 registers in place of 147, eight
 // waves a SIMD in place of three (us, one wave / three: 4096 x 1152 bf16 13.3 / 11.8, float32 to codes 32768 x 1152 98.1 / 98.2, one
@@ -687,6 +698,20 @@ hipError_t launch_block_norm(const NormArgs &a, bool stream_f32, bool params_f32
 {
     if (stream_f32) return params_f32 ? forward<float, float>(a, st) : forward<float, Bf16>(a, st);
     return params_f32 ? forward<Bf16, float>(a, st) : forward<Bf16, Bf16>(a, st);
+}
+
+hipError_t launch_zero_gradients(float *const (&grads)[7], const int64_t (&sizes)[7], hipStream_t st)
+{
+    ZeroArgs a{};
+    int64_t most = 0;
+    for (int i = 0; i < 7; ++i) {
+        a.to[i] = grads[i];
+        a.n[i] = grads[i] ? sizes[i] : 0;
+        most = std::max(most, a.n[i]);
+    }
+    if (most == 0) return hipSuccess;
+    block_norm_zero_kernel<<<dim3((unsigned)std::min<int64_t>((most + 255) / 256, 1024), 7), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
 }
 
 hipError_t launch_block_norm_bwd(const NormArgs &a, bool stream_f32, bool params_f32, hipStream_t st)

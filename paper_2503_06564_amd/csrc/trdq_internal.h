@@ -190,6 +190,7 @@ struct NormArgs {
 int norm_bwd_rows_per_group(int rows, int c, int64_t segments);
 int norm_bwd_groups(int rows, int c, int64_t segments);
 hipError_t launch_block_norm(const NormArgs &a, bool stream_f32, bool params_f32, hipStream_t st);
+hipError_t launch_zero_gradients(float *const (&grads)[7], const int64_t (&sizes)[7], hipStream_t st);
 hipError_t launch_block_norm_bwd(const NormArgs &a, bool stream_f32, bool params_f32, hipStream_t st);
 
 hipError_t launch_fp8_quant(const void *X, bool f32, int rows, int c, int64_t ldx, int blocks, bool e5m2, uint8_t *Q, int64_t ldq,

@@ -35,3 +35,23 @@ def test_gate_of_one_row_has_no_gradient_per_segment():
     assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate[0], dgate=torch.zeros(40), **kw) == accepted()
     assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate.contiguous(), dgate=torch.zeros(3, 40), **kw) == accepted()
     assert status(trdq.block_norm_bwd, X, X, X, X, gate=gate[:1], dgate=torch.zeros(1, 40), Y=X, ws=WS) == accepted()
+
+
+def test_no_rows_still_write_gradients():
+    """A sum over no rows is zero, and is written: only a call that has no gradient to write returns without a launch."""
+    none = X[:0]
+    vec, grad = torch.ones(40), torch.full((40,), 9.0)
+    trdq.block_norm_bwd(none, None, none, none, stream=0)
+    trdq.block_norm_bwd(none, None, none, none, pre_weight=vec, scale=torch.ones(1, 40), stream=0)
+    if torch.cuda.is_available():
+        return                                              # (tests/test_gpu_blocks_edges.py holds the values)
+    mods = torch.ones(3, 40)
+    off = torch.zeros(4, dtype=torch.int32)
+    assert status(trdq.block_norm_bwd, none, None, none, none, pre_weight=vec, dpre_weight=grad) == trdq.ERR_HIP
+    assert status(trdq.block_norm_bwd, none, none, none, none, Y=none, post="rms", post_weight=vec, dpost_weight=grad) == trdq.ERR_HIP
+    assert status(trdq.block_norm_bwd, none, none, none, none, Y=none, gate=vec, dgate=grad, seg_len=5) == trdq.ERR_HIP
+    for name in ("scale", "shift", "gate"):
+        kw = {name: mods, "d" + name: torch.full((3, 40), 9.0), "seg_off": off}
+        assert status(trdq.block_norm_bwd, none, none, none, none, Y=none, **kw) == trdq.ERR_HIP
+        trdq.block_norm_bwd(none, none, none, none, Y=none, seg_len=5, stream=0, **{name: mods[:0], "d" + name: mods[:0]})     # no segment either
+        assert status(trdq.block_norm_bwd, none, None, none, none, **{"d" + name: grad[None] if name != "gate" else grad}) == trdq.ERR_NULL
