@@ -537,7 +537,7 @@ __global__ __launch_bounds__(kJoinThreads) void block_norm_join_kernel(NormArgs 
             hi = max(0, min(hi, a.rows));
         }
         // (read here, ahead of the sums, which wait for memory too)
-        const bool writes = which == 0 && part == 0 && there;
+        const bool writes = which == 0 && part == 0 && there, some = hi > lo;
         const float scale = writes ? value_of<P>(a.scale, (int64_t)seg * a.ld_scale + k, 0.0f) : 0.0f;
         const float gate = writes ? value_of<P>(a.gate, (int64_t)seg * a.ld_gate + k, 1.0f) : 1.0f;
         const int g0 = lo / a.rows_per_group, g1 = there && hi > lo ? (hi - 1) / a.rows_per_group : -1;
@@ -559,19 +559,21 @@ __global__ __launch_bounds__(kJoinThreads) void block_norm_join_kernel(NormArgs 
         }
         const float sum[kNormSums] = {area[0][lane][cc], area[1][lane][cc], area[2][lane][cc], area[3][lane][cc]};
         if (writes) {
+            // (a segment without rows: zeros, whatever its parameters and the weights are: nothing was computed with them)
             const int64_t to = (int64_t)seg * a.c + k;
-            if (a.dscale) a.dscale[to] = __builtin_fmaf(w, sum[0], b * sum[1]);
+            if (a.dscale) a.dscale[to] = some ? __builtin_fmaf(w, sum[0], b * sum[1]) : 0.0f;
             if (a.dshift) a.dshift[to] = sum[1];
-            const float dgate = __builtin_fmaf(w2, sum[2], b2 * sum[3]);
-            if (a.dgate && a.gate_by_segment) a.dgate[to] = dgate;
-            all[0] += (1.0f + scale) * sum[0];
-            all[1] += (1.0f + scale) * sum[1];
-            if (a.gate_by_segment) {
-                all[2] += gate * sum[2];
-                all[3] += gate * sum[3];
-            } else {
-                all[2] += sum[2];
-                all[3] += sum[3];
+            if (a.dgate && a.gate_by_segment) a.dgate[to] = some ? __builtin_fmaf(w2, sum[2], b2 * sum[3]) : 0.0f;
+            if (some) {
+                all[0] += (1.0f + scale) * sum[0];
+                all[1] += (1.0f + scale) * sum[1];
+                if (a.gate_by_segment) {
+                    all[2] += gate * sum[2];
+                    all[3] += gate * sum[3];
+                } else {
+                    all[2] += sum[2];
+                    all[3] += sum[3];
+                }
             }
         }
     }
