@@ -100,6 +100,20 @@ float *gradient(PyObject *o, int64_t rows, int64_t c, const char *name)       //
     return static_cast<float *>(address(*t, name));
 }
 
+struct Workspace {
+    void *p = nullptr;
+    size_t bytes = 0;
+};
+
+// of any type and shape, but in one piece: its elements have to be the bytes behind its address
+Workspace workspace(PyObject *o)
+{
+    const at::Tensor *const t = tensor_of(o, "ws");
+    if (!t) return {};
+    if (!t->is_contiguous()) throw Bad{TRDQ_ERR_SHAPE, "ws: expected a contiguous tensor"};
+    return {address(*t, "ws"), (size_t)t->numel() * t->element_size()};
+}
+
 int64_t integer(PyObject *o)
 {
     const int64_t v = PyLong_AsLongLong(o);
@@ -165,7 +179,8 @@ PyObject *fp8_gemm(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 8, [&] {
         const at::Tensor &A = needed(a[0], "A"), &sa = needed(a[1], "sa"), &B = needed(a[2], "B"), &sb = needed(a[3], "sb"), &Y = needed(a[4], "Y");
-        const at::Tensor *const bias = tensor_of(a[5], "bias"), *const ws = tensor_of(a[6], "ws");
+        const at::Tensor *const bias = tensor_of(a[5], "bias");
+        const Workspace ws = workspace(a[6]);
         if (A.dim() != 2 || B.dim() != 2 || sb.dim() != 2) throw Bad{TRDQ_ERR_SHAPE, "A, B, sb: expected matrices"};
         const int64_t M = A.size(0), K = A.size(1), N = B.size(0), nkb = (K + 127) / 128, n_sb = (N + 127) / 128;
         if (K > INT32_MAX || N > INT32_MAX) throw Bad{TRDQ_ERR_UNSUPPORTED, "A, B: too large"};
@@ -175,8 +190,7 @@ PyObject *fp8_gemm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Matrix ma = matrix(&A, M, K, "A"), msa = matrix(&sa, nkb, M, "sa"), mb = matrix(&B, N, K, "B"), msb = matrix(&sb, nkb, tiles ? n_sb : N, "sb"),
                      y = matrix(&Y, M, N, "Y");
         return trdq_fp8_gemm(M, (int)N, (int)K, ma.p, type_of(A), ma.ld, msa.p, msa.ld, mb.p, type_of(B), mb.ld, msb.p, msb.ld, tiles, type_of(sa),
-                             static_cast<const float *>(vector(bias, N, "bias")), y.p, type_of(Y), y.ld, ws ? address(*ws, "ws") : nullptr,
-                             ws ? (size_t)ws->numel() * ws->element_size() : 0, stream_of(a[7]));
+                             static_cast<const float *>(vector(bias, N, "bias")), y.p, type_of(Y), y.ld, ws.p, ws.bytes, stream_of(a[7]));
     });
 }
 
@@ -276,7 +290,8 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     return guarded(n, 15 + kNormArgs, [&] {
         const at::Tensor &X = needed(a[2], "Xout");
         const at::Tensor *const dX = tensor_of(a[0], "dX"), *const dY = tensor_of(a[1], "dY"), *const dH = tensor_of(a[3], "dH"),
-                         *const Y = tensor_of(a[4], "Y"), *const dXo = tensor_of(a[5], "dXout"), *const ws = tensor_of(a[13], "ws");
+                         *const Y = tensor_of(a[4], "Y"), *const dXo = tensor_of(a[5], "dXout");
+        const Workspace ws = workspace(a[13]);
         int64_t segments = 0;
         const trdq_norm d = norm_of(X, a + 14, &segments);
         same_type(dX, X, "dX");
@@ -310,7 +325,7 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         g.dpre_bias_dev = gradient(a[10], -1, d.c, "dpre_bias");
         g.dpost_weight_dev = gradient(a[11], -1, d.c, "dpost_weight");
         g.dpost_bias_dev = gradient(a[12], -1, d.c, "dpost_bias");
-        return trdq_block_norm_bwd(&d, &g, ws ? address(*ws, "ws") : nullptr, ws ? (size_t)ws->numel() * ws->element_size() : 0, stream_of(a[14 + kNormArgs]));
+        return trdq_block_norm_bwd(&d, &g, ws.p, ws.bytes, stream_of(a[14 + kNormArgs]));
     });
 }
 

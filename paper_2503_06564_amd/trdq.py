@@ -793,7 +793,7 @@ def fp8_gemm_ws_nbytes(M, N, K):
 
 def fp8_gemm(A, sa, B, sb, Y, bias=None, ws=None, stream=None):
     """Y[m, n] (bf16 or float32) = sum over blocks of sa sb (A . B^T) + bias.  A [M, K] with sa [K / 128, M]; B [N, K] with sb
-    [K / 128, N], or [K / 128, ceil(N / 128)] (a scale per 128 x 128 tile).  ws: uint8 tensor of fp8_gemm_ws_nbytes(M, N, K)."""
+    [K / 128, N], or [K / 128, ceil(N / 128)] (a scale per 128 x 128 tile).  ws: contiguous uint8 tensor of fp8_gemm_ws_nbytes(M, N, K)."""
     bad = (_block_calls or _calls()).fp8_gemm(A, sa, B, sb, Y, bias, ws, stream)
     if bad:
         _refused(bad, "trdq_fp8_gemm")
@@ -819,7 +819,7 @@ def block_norm_bwd(dX, dY, Xout, dH, Y=None, dXout=None, dscale=None, dshift=Non
                    dpost_weight=None, dpost_bias=None, ws=None, pre="layer", pre_weight=None, pre_bias=None, scale=None, shift=None,
                    post=None, post_weight=None, post_bias=None, gate=None, eps=1e-6, seg_len=0, seg_off=None, stream=None):
     """Gradients of block_norm: dX (of X) and dY (of Y) from dXout (None: zero) and dH, where Xout is the stream as the norm read it; and
-    float32 gradients of those parameters whose tensor is given.  ws: uint8 tensor of block_norm_bwd_ws_nbytes(rows, c, segments)."""
+    float32 gradients of those parameters whose tensor is given.  ws: contiguous uint8 tensor of block_norm_bwd_ws_nbytes(rows, c, segments)."""
     bad = (_block_calls or _calls()).block_norm_bwd(dX, dY, Xout, dH, Y, dXout, dscale, dshift, dgate, dpre_weight, dpre_bias, dpost_weight,
                                                     dpost_bias, ws, NORM_KINDS.get(pre, -1), pre_weight, pre_bias, scale, shift,
                                                     NORM_KINDS.get(post, -1), post_weight, post_bias, gate, eps, seg_len, seg_off, stream)

@@ -55,3 +55,20 @@ def test_no_rows_still_write_gradients():
         assert status(trdq.block_norm_bwd, none, none, none, none, Y=none, **kw) == trdq.ERR_HIP
         trdq.block_norm_bwd(none, none, none, none, Y=none, seg_len=5, stream=0, **{name: mods[:0], "d" + name: mods[:0]})     # no segment either
         assert status(trdq.block_norm_bwd, none, None, none, none, **{"d" + name: grad[None] if name != "gate" else grad}) == trdq.ERR_NULL
+
+
+def test_workspaces_own_what_they_count():
+    """An expanded or strided workspace owns fewer bytes than it has elements, or not those that lie behind its address."""
+    vec = dict(pre_weight=torch.ones(40), dpre_weight=torch.zeros(40))
+    a, b = (torch.zeros(n, 4608, dtype=torch.uint8).view(torch.float8_e4m3fn) for n in (300, 1152))
+    sa, sb, y = torch.ones(36, 300), torch.ones(36, 1152), torch.zeros(300, 1152)
+    need = trdq.fp8_gemm_ws_nbytes(300, 1152, 4608)
+    assert need > 0
+    for n, f, args, kw in ((trdq.block_norm_bwd_ws_nbytes(6, 40, 1), trdq.block_norm_bwd, (X, None, X, X), vec),
+                           (need, trdq.fp8_gemm, (a, sa, b, sb, y), {})):
+        whole = torch.zeros(2 * n, dtype=torch.uint8)
+        for ws in (whole[:1].expand(n), whole[::2], whole[:n].view(2, n // 2).t()):
+            assert ws.numel() >= n and status(f, *args, ws=ws, **kw) == trdq.ERR_SHAPE
+        assert status(f, *args, ws=whole[:n - 1], **kw) == trdq.ERR_SHAPE
+        assert status(f, *args, ws=whole[:n], **kw) == accepted()
+        assert status(f, *args, ws=whole[:n].view(torch.float32)[None], **kw) == accepted()
