@@ -41,7 +41,8 @@ trdq_status check_norm(const trdq_norm *n, int64_t *segments_out)
     if ((n->pre != TRDQ_NORM_LAYER && n->pre != TRDQ_NORM_RMS) || n->post < TRDQ_NORM_NONE || n->post > TRDQ_NORM_RMS) return TRDQ_ERR_RANGE;
     if (!(n->eps >= 0.0f) || std::isinf(n->eps) || n->seg_len < 0 || (n->seg_len == 0 && n->seg_off && n->n_seg <= 0)) return TRDQ_ERR_RANGE;
     if (n->seg_len == 0 && n->seg_off && !aligned(n->seg_off, 4)) return TRDQ_ERR_SHAPE;
-    const int64_t segments = n->seg_len > 0 ? (n->rows + n->seg_len - 1) / n->seg_len : n->seg_off ? n->n_seg : 1;
+    // (rows + seg_len may not fit 64 bits)
+    const int64_t segments = n->seg_len > 0 ? n->rows / n->seg_len + (n->rows % n->seg_len != 0) : n->seg_off ? n->n_seg : 1;
     const size_t size = size_of(n->param_dtype);
     const void *const vectors[] = {n->pre_weight, n->pre_bias, n->post_weight, n->post_bias, n->scale, n->shift, n->gate};
     for (const void *v : vectors)

@@ -214,7 +214,7 @@ trdq_norm norm_of(const at::Tensor &X, PyObject *const *a, int64_t *segments_out
     d.seg_len = integer(a[10]);
     int64_t segments = 1;
     if (d.seg_len > 0) {
-        segments = (d.rows + d.seg_len - 1) / d.seg_len;
+        segments = d.rows / d.seg_len + (d.rows % d.seg_len != 0);          // (their sum may not fit 64 bits)
     } else if (const at::Tensor *const off = tensor_of(a[11], "seg_off")) {
         if (off->dim() != 1 || off->scalar_type() != at::kInt || off->size(0) > INT32_MAX) throw Bad{TRDQ_ERR_SHAPE, "seg_off: expected an int32 vector"};
         segments = off->size(0) - 1;

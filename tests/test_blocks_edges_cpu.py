@@ -72,3 +72,15 @@ def test_workspaces_own_what_they_count():
         assert status(f, *args, ws=whole[:n - 1], **kw) == trdq.ERR_SHAPE
         assert status(f, *args, ws=whole[:n], **kw) == accepted()
         assert status(f, *args, ws=whole[:n].view(torch.float32)[None], **kw) == accepted()
+
+
+@pytest.mark.parametrize("seg_len", [6, 7, 2 ** 31, 2 ** 62, 2 ** 63 - 6, 2 ** 63 - 2, 2 ** 63 - 1])
+def test_segments_longer_than_the_rows(seg_len):
+    """One segment, however long it could be; its workspace is that of one segment."""
+    mods, grad = torch.ones(1, 40), torch.zeros(1, 40)
+    need = trdq.block_norm_bwd_ws_nbytes(6, 40, 1)
+    assert status(trdq.block_norm, X, None, X, scale=mods, seg_len=seg_len) == accepted()
+    args = (X, None, X, X)
+    assert status(trdq.block_norm_bwd, *args, scale=mods, dscale=grad, seg_len=seg_len, ws=WS[:need]) == accepted()
+    assert status(trdq.block_norm_bwd, *args, scale=mods, dscale=grad, seg_len=seg_len, ws=WS[:need - 4]) == trdq.ERR_SHAPE
+    assert status(trdq.block_norm_bwd, *args, pre_weight=mods[0], dpre_weight=grad[0], seg_len=seg_len, ws=WS[:need - 4]) == trdq.ERR_SHAPE
