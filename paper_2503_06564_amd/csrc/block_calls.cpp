@@ -217,6 +217,7 @@ trdq_norm norm_of(const at::Tensor &X, PyObject *const *a, int64_t *segments_out
         segments = d.rows / d.seg_len + (d.rows % d.seg_len != 0);          // (their sum may not fit 64 bits)
     } else if (const at::Tensor *const off = tensor_of(a[11], "seg_off")) {
         if (off->dim() != 1 || off->scalar_type() != at::kInt || off->size(0) > INT32_MAX) throw Bad{TRDQ_ERR_SHAPE, "seg_off: expected an int32 vector"};
+        if (off->size(0) < 2) throw Bad{TRDQ_ERR_RANGE, "seg_off: expected two borders at least"};       // (none has no address: no borders)
         segments = off->size(0) - 1;
         d.n_seg = (int)segments;
         d.seg_off = static_cast<const int32_t *>(vector(off, segments + 1, "seg_off"));

@@ -84,3 +84,12 @@ def test_segments_longer_than_the_rows(seg_len):
     assert status(trdq.block_norm_bwd, *args, scale=mods, dscale=grad, seg_len=seg_len, ws=WS[:need]) == accepted()
     assert status(trdq.block_norm_bwd, *args, scale=mods, dscale=grad, seg_len=seg_len, ws=WS[:need - 4]) == trdq.ERR_SHAPE
     assert status(trdq.block_norm_bwd, *args, pre_weight=mods[0], dpre_weight=grad[0], seg_len=seg_len, ws=WS[:need - 4]) == trdq.ERR_SHAPE
+
+
+@pytest.mark.parametrize("borders", [0, 1])
+def test_borders_of_no_segment_are_refused(borders):
+    off = torch.zeros(borders, dtype=torch.int32)
+    for x in (X, X[:0]):
+        assert status(trdq.block_norm, x, None, x, seg_off=off) == trdq.ERR_RANGE
+        assert status(trdq.block_norm, x, None, x, scale=torch.ones(1, 40), seg_off=off) == trdq.ERR_RANGE
+        assert status(trdq.block_norm_bwd, x, None, x, x, seg_off=off) == trdq.ERR_RANGE
