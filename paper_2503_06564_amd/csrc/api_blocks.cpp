@@ -164,7 +164,7 @@ trdq_status trdq_block_norm(const trdq_norm *n, const void *X_dev, int64_t ldx, 
 
 size_t trdq_block_norm_bwd_ws_nbytes(int64_t rows, int c, int64_t segments)
 {
-    if (rows <= 0 || rows >= kMostRows || c <= 0 || c > kMostNormChannels || segments <= 0) return 0;
+    if (rows <= 0 || rows >= kMostRows || c <= 0 || c > kMostNormChannels || segments <= 0 || segments > 0x7FFFFFFF) return 0;
     return (size_t)(trdq::norm_bwd_groups((int)rows, c, segments) + segments) * trdq::kNormSums * c * sizeof(float);
 }
 

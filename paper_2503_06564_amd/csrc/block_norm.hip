@@ -301,7 +301,7 @@ __global__ __launch_bounds__(W == 1 ? 64 * kBwdWaves : 64 * W) void block_norm_b
     const int r_in = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const Row<W, NCH> row{(int)threadIdx.x - 64 * r_in, a.c};
     RowSums<W> sums{area};
-    const int begin = (int)blockIdx.x * a.rows_per_group, end = min(a.rows, begin + a.rows_per_group);
+    const int begin = (int)blockIdx.x * a.rows_per_group, end = begin + min(a.rows - begin, a.rows_per_group);
     const bool pre_layer = a.pre == TRDQ_NORM_LAYER, post_layer = a.post == TRDQ_NORM_LAYER;
 
     int seg = a.by_segment ? segment_of(a, begin) : 0;
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(W == 1 ? 64 * kBwdWaves : 64 * W) void block_norm_b
         }
         // the sums of this workgroup's rows of the segment
         if (a.part) {
-            float *const to = a.part + (int64_t)((int)blockIdx.x + seg) * kNormSums * a.c;
+            float *const to = a.part + ((int64_t)blockIdx.x + seg) * kNormSums * a.c;
             auto put = [&](int which, float (&v)[NCH][8]) {
                 if constexpr (W == 1) {
                     // the upper half of the waves hands its sums to the lower half, whose sums are then added
@@ -546,7 +546,7 @@ __global__ __launch_bounds__(kJoinThreads) void block_norm_join_kernel(NormArgs 
             for (int g = g0 + part; g <= g1; g += 8 * per) {
                 float v[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = a.part[((int64_t)(min(g + u * per, g1) + seg) * kNormSums + which) * a.c + k];
+                for (int u = 0; u < 8; ++u) v[u] = a.part[(((int64_t)min(g + u * per, g1) + seg) * kNormSums + which) * a.c + k];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) add += g + u * per <= g1 ? v[u] : 0.0f;
             }
@@ -684,16 +684,17 @@ hipError_t backward(const NormArgs &a, hipStream_t st)
 int norm_bwd_rows_per_group(int rows, int c, int64_t segments)
 {
     const bool waves = c <= 1536;
-    const int most = (c > 512 && waves) || c > 4096 ? 256 : 512, least = (rows + most - 1) / most;
+    // (in 64 bits: rows may be all but 2^31)
+    const int64_t most = (c > 512 && waves) || c > 4096 ? 256 : 512, least = (rows + most - 1) / most;
     const int64_t segment = (rows + segments - 1) / segments;
-    const int per = std::max(least, waves ? (int)std::min<int64_t>(segment, kBwdWaves) : 1);
-    return per < kBwdWaves ? per : waves ? (per + kBwdWaves - 1) / kBwdWaves * kBwdWaves : per;
+    const int64_t per = std::max<int64_t>(least, waves ? std::min<int64_t>(segment, kBwdWaves) : 1);
+    return (int)(per < kBwdWaves || !waves ? per : (per + kBwdWaves - 1) / kBwdWaves * kBwdWaves);
 }
 
 int norm_bwd_groups(int rows, int c, int64_t segments)
 {
-    const int per = norm_bwd_rows_per_group(rows, c, segments);
-    return (rows + per - 1) / per;
+    const int64_t per = norm_bwd_rows_per_group(rows, c, segments);
+    return (int)((rows + per - 1) / per);
 }
 
 hipError_t launch_block_norm(const NormArgs &a, bool stream_f32, bool params_f32, hipStream_t st)

@@ -93,3 +93,15 @@ def test_borders_of_no_segment_are_refused(borders):
         assert status(trdq.block_norm, x, None, x, seg_off=off) == trdq.ERR_RANGE
         assert status(trdq.block_norm, x, None, x, scale=torch.ones(1, 40), seg_off=off) == trdq.ERR_RANGE
         assert status(trdq.block_norm_bwd, x, None, x, x, seg_off=off) == trdq.ERR_RANGE
+
+
+@pytest.mark.parametrize("c", [1, 600, 1152, 4608, 16384])
+def test_workspace_of_norm_gradients_is_bounded(c):
+    """At most 512 runs (and as many as rows) beside the segments, four float32 sums each, up to the last row count that is accepted."""
+    for rows in (1, 7, 8, 9, 511, 512, 513, 4095, 4097, 2 ** 20 + 1, 2 ** 30 + 3, 2 ** 31 - 4096, 2 ** 31 - 1000, 2 ** 31 - 300, 2 ** 31 - 258):
+        for segments in (1, 2, 64, 4096, 2 ** 31 - 1):
+            need = trdq.block_norm_bwd_ws_nbytes(rows, c, segments)
+            assert (1 + segments) * 16 * c <= need <= (min(rows, 512) + segments) * 16 * c, (rows, segments)
+    # sizes that no call takes
+    for rows, width, segments in ((2 ** 31 - 256, c, 1), (0, c, 1), (5, 16385, 1), (5, c, 0), (5, c, 2 ** 31), (5, c, 2 ** 63 - 1)):
+        assert trdq.block_norm_bwd_ws_nbytes(rows, width, segments) == 0
