@@ -5,7 +5,7 @@
 
 namespace {
 
-constexpr int64_t kMostRows = 0x7FFFFFFF - 256;
+constexpr int64_t kMostRows = 0x80000000 - 256;           // refused from here on: rows of a tile behind the last still count in 31 bits
 constexpr int kMostNormChannels = 16384;
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }

@@ -1,5 +1,7 @@
 """Calls around a block's linears at the edges of what they accept, without a GPU: what is refused, and sizes that the library computes on
 the host.  (Without a device a call whose arguments are right ends in ERR_HIP: nothing can be launched.)"""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -105,3 +107,19 @@ def test_workspace_of_norm_gradients_is_bounded(c):
     # sizes that no call takes
     for rows, width, segments in ((2 ** 31 - 256, c, 1), (0, c, 1), (5, 16385, 1), (5, c, 0), (5, c, 2 ** 31), (5, c, 2 ** 63 - 1)):
         assert trdq.block_norm_bwd_ws_nbytes(rows, width, segments) == 0
+
+
+def test_most_rows():
+    """Fewer than 2^31 - 256 rows are taken (a call without addresses gets as far as ERR_NULL), that many are not."""
+    L, norm = trdq.lib(), trdq._Norm(c=40, x_dtype=trdq.BF16, param_dtype=trdq.F32, pre=1, post=0, eps=1e-6)
+    calls = {
+        "fp8_quant": lambda rows: L.trdq_fp8_quant(None, trdq.BF16, rows, 40, 40, 0, trdq.E4M3, None, 128, trdq.F32, None, rows, None),
+        "fp8_gemm": lambda rows: L.trdq_fp8_gemm(rows, 40, 128, None, trdq.E4M3, 128, None, rows, None, trdq.E4M3, 128, None, 40, 0, trdq.F32, None, None,
+                                                 trdq.BF16, 40, None, 0, None),
+        "block_norm": lambda rows: L.trdq_block_norm(C.byref(norm), None, 40, None, 0, None, 0, trdq.BF16, None, 40, 0, None, 0, None),
+        "block_norm_bwd": lambda rows: L.trdq_block_norm_bwd(C.byref(norm), C.byref(trdq._NormGrads()), None, 0, None)}
+    for name, call in calls.items():
+        for rows, want in ((2 ** 31 - 257, trdq.ERR_NULL), (2 ** 31 - 256, trdq.ERR_UNSUPPORTED)):
+            norm.rows = rows
+            assert call(rows) == want, (name, rows)
+    assert trdq.block_norm_bwd_ws_nbytes(2 ** 31 - 257, 40, 1) > 0
