@@ -133,7 +133,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_kernel(NormA
     constexpr int kRows = W == 1 ? 4 : 1;              // of a workgroup
     __shared__ float area[2][2 * W];
     const int r_in = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-    const int row_i = (int)blockIdx.x * kRows + r_in;
+    const int row_i = a.first + (int)blockIdx.x * kRows + r_in;
     if (row_i >= a.rows) return;
     const Row<W, NCH> row{(int)threadIdx.x - 64 * r_in, a.c};
     RowSums<W> sums{area};
@@ -629,14 +629,20 @@ hipError_t by_width(int c, F &&f)
 }
 
 template <class T, class P>
-hipError_t forward(const NormArgs &a, hipStream_t st)
+hipError_t forward(NormArgs a, hipStream_t st)
 {
     // (codes are written up to the end of the last block)
     return by_width<true>(a.out == TRDQ_E4M3 ? a.nkb * 128 : a.c, [&](auto w, auto nch) {
         constexpr int W = decltype(w)::value, NCH = decltype(nch)::value;
-        const unsigned grid = W == 1 ? (unsigned)(((int64_t)a.rows + 3) / 4) : (unsigned)a.rows;
-        block_norm_kernel<T, P, W, NCH><<<dim3(grid), dim3(W == 1 ? 256 : 64 * W), 0, st>>>(a);
-        return hipGetLastError();
+        constexpr int kRows = W == 1 ? 4 : 1, kThreads = W == 1 ? 256 : 64 * W;
+        constexpr int64_t kAtOnce = kMostThreads / kThreads * kRows;
+        for (int64_t first = 0; first < a.rows; first += kAtOnce) {
+            a.first = (int)first;
+            const int64_t n = std::min(a.rows - first, kAtOnce);
+            block_norm_kernel<T, P, W, NCH><<<dim3((unsigned)((n + kRows - 1) / kRows)), dim3(kThreads), 0, st>>>(a);
+            if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        return hipSuccess;
     });
 }
 

@@ -2,6 +2,8 @@
 //   top = max |x| of the block (at least 2^-100),  s = top / max,  code = nearest value of the format to x / s
 // or, with scales as powers of two, s = the smallest 2^e >= top / max.  Blocks lie along a row (rows), down a column (cols, codes
 // transposed) or are 128 x 128 tiles (tiles, tiles_t).  Every value is read once and its code written once; memory bounds all four.
+#include <algorithm>
+
 #include "fp8_common.h"
 
 namespace trdq {
@@ -19,6 +21,7 @@ struct QuantArgs {
     int rows, c;               // of X
     int nkb;                   // blocks along the codes' rows
     int groups;                // rows: groups of KT blocks; turned forms: column tiles
+    int first;                 // rows: the launch's first row
 };
 
 // A workgroup takes 32 rows x KT blocks of 128, 16 lanes to a block: a wave's load covers four blocks' 256 (bf16) bytes, and all of a
@@ -28,7 +31,7 @@ template <class T, int FMT, bool POW2, int KT>
 __global__ __launch_bounds__(kThreads) void quant_rows_kernel(QuantArgs a)
 {
     __shared__ uint32_t scales[KT * 32];
-    const int group = blockIdx.x % a.groups, row0 = (int)(blockIdx.x / a.groups) * 32;
+    const int group = blockIdx.x % a.groups, row0 = a.first + (int)(blockIdx.x / a.groups) * 32;
     const int kb0 = group * KT, p = threadIdx.x & 15, g = threadIdx.x >> 4;
     Piece<T> in[2 * KT];
 #pragma unroll
@@ -188,14 +191,18 @@ hipError_t launch(QuantArgs a, int blocks, hipStream_t st)
             // the blocks of a row in groups of up to four, of equal size (9 = 3 x 3: a group of one would leave lanes idle)
             a.groups = (a.nkb + 3) / 4;
             const int kt = (a.nkb + a.groups - 1) / a.groups;
-            const int64_t grid = (int64_t)a.groups * ((a.rows + 31) / 32);
-            if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-            const dim3 g((unsigned)grid), t(kThreads);
-            if (kt == 1) quant_rows_kernel<T, FMT, POW2, 1><<<g, t, 0, st>>>(a);
-            else if (kt == 2) quant_rows_kernel<T, FMT, POW2, 2><<<g, t, 0, st>>>(a);
-            else if (kt == 3) quant_rows_kernel<T, FMT, POW2, 3><<<g, t, 0, st>>>(a);
-            else quant_rows_kernel<T, FMT, POW2, 4><<<g, t, 0, st>>>(a);
-            break;
+            const int64_t at_once = kMostThreads / kThreads / a.groups * 32;
+            for (int64_t first = 0; first < a.rows; first += at_once) {
+                a.first = (int)first;
+                const int64_t n = std::min(a.rows - first, at_once);
+                const dim3 g((unsigned)(a.groups * ((n + 31) / 32))), t(kThreads);
+                if (kt == 1) quant_rows_kernel<T, FMT, POW2, 1><<<g, t, 0, st>>>(a);
+                else if (kt == 2) quant_rows_kernel<T, FMT, POW2, 2><<<g, t, 0, st>>>(a);
+                else if (kt == 3) quant_rows_kernel<T, FMT, POW2, 3><<<g, t, 0, st>>>(a);
+                else quant_rows_kernel<T, FMT, POW2, 4><<<g, t, 0, st>>>(a);
+                if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+            }
+            return hipSuccess;
         }
         case TRDQ_BLOCKS_TILES:
             quant_tiles_kernel<T, FMT, POW2><<<dim3((unsigned)((int64_t)row_tiles * col_tiles)), dim3(kThreads), 0, st>>>(a);
@@ -224,7 +231,7 @@ hipError_t launch_fp8_quant(const void *X, bool f32, int rows, int c, int64_t ld
                             void *S, int64_t lds, bool pow2, hipStream_t st)
 {
     const bool turned = blocks == TRDQ_BLOCKS_COLS || blocks == TRDQ_BLOCKS_TILES_T;
-    QuantArgs a{X, Q, S, ldx, ldq, lds, rows, c, ((turned ? rows : c) + 127) / 128, 0};
+    QuantArgs a{X, Q, S, ldx, ldq, lds, rows, c, ((turned ? rows : c) + 127) / 128, 0, 0};
     return f32 ? launch_from<float>(a, blocks, e5m2, pow2, st) : launch_from<Bf16>(a, blocks, e5m2, pow2, st);
 }
 

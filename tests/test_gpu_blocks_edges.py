@@ -91,3 +91,68 @@ def test_parameters_of_empty_segments_reach_nothing(off, c, post):
         for k in ("dscale", "dshift", "dgate"):
             assert bool((got[k].cpu()[empty] == 0).all()), k
         assert bool(got["dpre_bias"].isfinite().all())
+
+
+# A dispatch counts its threads in 32 bits: calls of more rows are several.  Their rows are checked on both sides of that.
+
+def test_norm_of_more_rows_than_a_launch_takes():
+    """8 channels (four rows a workgroup of 256 threads: 2^26 - 4 rows a launch), modulated by segments of 2^25 rows."""
+    rows, c, seg_len = 2 ** 26 + 37, 8, 2 ** 25
+    at = torch.tensor([0, 1, 2 ** 25 - 1, 2 ** 25, 2 ** 26 - 5, 2 ** 26 - 4, 2 ** 26 - 3, 2 ** 26 - 1, 2 ** 26, rows - 1])
+    mods = (rand(1, 3, 2 * c) * 0.3).to(dev())
+    X, H = (torch.zeros(rows, c, dtype=torch.bfloat16, device=dev()) for _ in range(2))
+    X[at.to(dev())] = rand(2, len(at), c).to(dev()).to(torch.bfloat16)
+    H.fill_(7.0)
+    trdq.block_norm(X, None, H, shift=mods[:, :c], scale=mods[:, c:], seg_len=seg_len)
+    torch.cuda.synchronize()
+    o = ref.BlockNorm({"shift": mods[:, :c].cpu().double(), "scale": mods[:, c:].cpu().double()}, at // seg_len, "layer", None, 1e-6)
+    x, got = X[at.to(dev())].cpu().double(), H[at.to(dev())].cpu().double()
+    assert bool(((got - o.out(x)).abs() <= 128 * 2.0 ** -24 * o.out_size(x) + 2.0 ** -8 * 1.01 * o.out(x).abs()).all())
+    # every other row is zeros in, its segment's shift out
+    for s in range(3):
+        part = H[s * seg_len:(s + 1) * seg_len]
+        same = (part == mods[s, :c].to(torch.bfloat16)).all(1)
+        assert int((~same).sum()) <= len(at)
+
+
+def test_norm_of_more_wide_rows_than_a_launch_takes():
+    """1032 channels (a workgroup of 192 threads a row: 22369621 rows a launch), to bf16 and to codes of another row count."""
+    c, at_once = 1032, 2 ** 32 // 192
+    rows = at_once + 9
+    X = torch.empty(rows, c, dtype=torch.bfloat16, device=dev())
+    x = rand(3, 12, c).to(torch.bfloat16)
+    X[-12:].copy_(x)
+    H = torch.empty(rows, c, dtype=torch.bfloat16, device=dev())
+    trdq.block_norm(X, None, H, pre="rms")
+    few, fewer = torch.empty(12, c, dtype=torch.bfloat16, device=dev()), X[-12:].clone()
+    trdq.block_norm(fewer, None, few, pre="rms")
+    torch.cuda.synchronize()
+    assert torch.equal(H[-12:], few)
+    del H
+    Q = torch.empty(rows, 1152, dtype=torch.uint8, device=dev()).view(torch.float8_e4m3fn)
+    S = torch.empty(9, rows, device=dev())
+    trdq.block_norm(X, None, None, codes=Q, code_scales=S, pre="rms")
+    Q2, S2 = torch.empty(12, 1152, dtype=torch.uint8, device=dev()).view(torch.float8_e4m3fn), torch.empty(9, 12, device=dev())
+    trdq.block_norm(fewer, None, None, codes=Q2, code_scales=S2, pre="rms")
+    torch.cuda.synchronize()
+    assert torch.equal(Q[-12:].view(torch.uint8), Q2.view(torch.uint8)) and torch.equal(S[:, -12:], S2)
+    del X, Q, S
+    torch.cuda.empty_cache()
+
+
+def test_codes_of_more_rows_than_a_launch_takes():
+    """One channel (32 rows a workgroup of 256 threads: 2^29 - 32 rows a launch)."""
+    rows = 2 ** 29 + 75
+    X = torch.ones(rows, 1, dtype=torch.bfloat16, device=dev())
+    tail = rand(4, 200, 1).to(torch.bfloat16)
+    X[-200:].copy_(tail)
+    Q = torch.empty(rows, 128, dtype=torch.uint8, device=dev()).view(torch.float8_e4m3fn)
+    S = torch.empty(1, rows, device=dev())
+    trdq.fp8_quant(X, Q, S)
+    torch.cuda.synchronize()
+    want, s, _ = ref.quant(tail, "rows", "e4m3", False)
+    assert torch.equal(Q[-200:].cpu().float().double(), want) and torch.equal(S[:, -200:].cpu().double(), s.float().double())
+    one = torch.tensor(1.0) / 448.0
+    assert bool((S[:, :-200] == one.item()).all()) and bool((Q[:-200, 0].view(torch.uint8) == 0x7E).all())
+    del X, Q, S
+    torch.cuda.empty_cache()
