@@ -163,12 +163,11 @@ hipError_t launch_linear_fused(const Weights &w, const uint16_t *X, int64_t M, i
                                hipStream_t st, bool asym = false);
 
 // ---- around a block's linears (block_norm.hip, fp8_quant.hip, fp8_gemm.hip) ----
-// A dispatch counts its threads in 32 bits: calls of more rows are several launches.
+// A dispatch counts the threads of each grid dimension in 32 bits.
 constexpr int64_t kMostThreads = 0xFFFFFFFF;
 // Both directions of the block norm; see trdq_norm and trdq_norm_grads.
 constexpr int kNormSums = 4;     // sums over a segment's rows that the parameters' gradients are made of
 struct NormArgs {
-    int first;                   // row of the launch's first workgroup (forward)
     const void *X, *Y;           // the stream (backward: as the norm read it) and the branch
     void *Xout, *H;
     uint8_t *Q;                  // codes in place of H
