@@ -509,8 +509,8 @@ typedef enum trdq_dtype {
 } trdq_dtype;
 
 /* trdq_fp8_quant: codes of X (bf16 or float32 [rows, c], row stride ldx >= c, aligned to its values).
- *   top = max |x| over a block, at least 2^-100;  code = the nearest value of the format to x / s, ties to even;
- *   s = top / max (float32), or the smallest 2^e >= top / max (e8m0).
+ *   top = max |x| over a block, at least 2^-100;  s = top / max (float32), or the smallest 2^e >= top / max (e8m0);
+ *   code = the nearest value of the format to x / s (to x max / top, exactly, not to x by the rounded s), ties to even.
  *   blocks               codes Q               scales S
  *   TRDQ_BLOCKS_ROWS     [rows, up(c)]         [up(c) / 128, rows]                       128 values of a row
  *   TRDQ_BLOCKS_COLS     [c, up(rows)]         [up(rows) / 128, c]                       128 values of a column, codes transposed
@@ -574,7 +574,8 @@ typedef struct trdq_norm {
 
 /* trdq_block_norm: X [rows, c] stream, Y [rows, c] bf16 or NULL (no branch: Xout is NULL too), Xout (may be X), and h_dtype
  * BF16 or F32: H [rows, c]; E4M3: codes H [rows, up(c)] (ldh a multiple of 16, 16-byte aligned) with S [up(c) / 128, rows] of
- * s_dtype F32 or E8M0 and row stride lds, as trdq_fp8_quant(ROWS) makes them of h in float32.  Row strides in values, >= c; bases
+ * s_dtype F32 or E8M0 and row stride lds, as trdq_fp8_quant(ROWS) makes them of h in float32 (with F32 scales each of a quotient
+ * h / s that is off by 2^-22 of itself at most: h has roundings of that size).  Row strides in values, >= c; bases
  * aligned to their values.  rows == 0 is a no-op.
  * Errors: NULL -> ERR_NULL; sizes, strides, alignment, Y without Xout or Xout without Y -> ERR_SHAPE; pre or post unknown, pre
  * NONE, eps negative or NaN, seg_len < 0, n_seg <= 0 with seg_off -> ERR_RANGE; another type, c > 16384, rows >= 2^31 - 256

@@ -167,13 +167,12 @@ __device__ __forceinline__ uint32_t row16_umax(uint32_t x)
     return x;
 }
 
-// What a block's largest magnitude makes of it.  Scales in float32: s = top / max, and a value's code is the nearest to the exact
-// x max / top, ties to even: values of bf16 do fall on a border between two codes (x max / top is a short fraction for many
-// pairs), and a rounded quotient would move them off it.  With t = 0.875 x (exact for bf16, and no overflow) and top2 = top /
-// 2^TopExp, q0 = t rc is within two steps of t / top2 and one step of the residual, fma(t - q0 top2, rc, q0), gives the nearest
-// float, which for a quotient on a border is the border.  Scales as powers of two (e8m0): the smallest that is at least top / max,
-// undone exactly.  A block whose largest magnitude is Inf or NaN gets a NaN as its scale and as its codes; one of zeros (or of
-// values below 2^-100) the scale of 2^-100.
+// What a block's largest magnitude makes of it.  Scales in float32: s = top / max; a value is divided by it as x max / top: with t =
+// 0.875 x (no overflow) and top2 = top / 2^TopExp, q0 = t rc is within two steps of t / top2, and one step of the residual,
+// fma(t - q0 top2, rc, q0), leaves a float32 rounding or two (2^-22) of the quotient.  That is for values that carry such roundings
+// themselves, as a norm's; the quantiser has to give the nearest code (fp8_quant.hip).  Scales as powers of two (e8m0): the smallest
+// that is at least top / max, undone exactly.  A block whose largest magnitude is Inf or NaN gets a NaN as its scale and as its codes;
+// one of zeros (or of values below 2^-100) the scale of 2^-100.
 struct BlockScale {
     float rc, top2;            // float32 scales: 1 / top2 and top2; e8m0: the factor 2^-e, and 0
     float s;                   // float32 scale

@@ -1,5 +1,5 @@
 // Codes in 8-bit floating point with a scale per block of 128 values:
-//   top = max |x| of the block (at least 2^-100),  s = top / max,  code = nearest value of the format to x / s
+//   top = max |x| of the block (at least 2^-100),  s = top / max,  code = nearest value of the format to x max / top
 // or, with scales as powers of two, s = the smallest 2^e >= top / max.  Blocks lie along a row (rows), down a column (cols, codes
 // transposed) or are 128 x 128 tiles (tiles, tiles_t).  Every value is read once and its code written once; memory bounds all four.
 #include <algorithm>
@@ -23,6 +23,71 @@ struct QuantArgs {
     int groups;                // rows: groups of KT blocks; turned forms: column tiles
     int first;                 // rows: the launch's first row
 };
+
+// ---- the nearest code -----------------------------------------------------------------------------
+// A value's code is the nearest to the exact quotient x max / top, ties to even.  Both are brought next to 1 by a power of two (no step
+// overflows, and none of those that decide about a code underflows): with t = 0.875 x and top2 = top / 2^TopExp, q0 = t rc is within
+// two steps of t / top2 and one step of the residual, fma(t - q0 top2, rc, q0), gives the nearest float.
+//   x of bf16: t is exact, and quotients that are no border between two codes are further from it than a float's rounding (x max and
+//   top have 11 and 8 bits): the nearest float is on a border where the quotient is, which many are.
+//   x of float32: t leaves a remainder tl, which joins the residual, and a quotient may be that near to a border without being on
+//   it.  So a float that is not the quotient gives its place to the one of its two neighbours around the quotient that is odd: borders
+//   have few bits, are even, and none lies between it and the quotient.  (The sign of what is left is right: where the fma
+//   has more than 24 bits, tl is at most half of it.)  Most values need none of that: x k (1 - 2^-20) and x k (1 + 2^-20), with k within
+//   2^-21 of max / top, lie on both sides of the quotient, and where they have the same code so has it; one value in 2^15 does not
+//   (by rows, us, all steps for every value / so: 16384 x 1152 19.2 / 16.4, 1003 x 771 5.9 / 5.1; bf16 values, many on borders, 5.4 / 6.1
+//   at 4096 x 1152).
+struct Divisor {
+    float rc, top2, pre;       // 1 / top2, top2 and 0.875, the latter two times the power; e8m0: the factor 2^-e, 0, 0
+
+    template <int FMT, bool POW2>
+    __device__ __forceinline__ static Divisor of(uint32_t top_bits, const BlockScale &b)
+    {
+        if constexpr (POW2) return {b.rc, 0.0f, 0.0f};
+        const float nan = __uint_as_float(0x7FC00000u);
+        const bool bad = top_bits >= 0x7F800000u;
+        top_bits = umax(top_bits, (uint32_t)(127 - 100) << 23);
+        const float power = __uint_as_float((256u - (top_bits >> 23)) << 23);                     // top power lies in [4, 8)
+        const float top2 = __uint_as_float(top_bits) * power * (TopExp<FMT>::value == 9 ? 0x1p-9f : 0x1p-16f);
+        const float r = __builtin_amdgcn_rcpf(top2);
+        return {bad ? nan : __builtin_fmaf(__builtin_fmaf(-top2, r, 1.0f), r, r), top2, 0.875f * power};
+    }
+
+    template <bool POW2, bool F32>
+    __device__ __forceinline__ float quotient(float x) const
+    {
+        if constexpr (POW2) return x * rc;
+        const float t = x * pre, q0 = t * rc, r = __builtin_fmaf(-q0, top2, t);
+        if constexpr (!F32) return __builtin_fmaf(r, rc, q0);
+        const float tl = __builtin_fmaf(x, pre, -t);
+        const float q = __builtin_fmaf(r + tl, rc, q0);
+        const uint32_t bits = __float_as_uint(q), rest = __float_as_uint(__builtin_fmaf(-q, top2, t) + tl);      // (+0 where nothing is left)
+        const uint32_t some = rest < 1u ? rest : 1u, beyond = (uint32_t)((int32_t)(bits ^ rest) >> 31) & some;
+        return __uint_as_float((bits - beyond) | some);
+    }
+    __device__ __forceinline__ float about() const { return rc * pre; }      // max / top, float32 scales
+};
+
+// The codes of eight values of a block.  about: of its divisor, for float32 values and scales; divisor(): itself, where it is needed.
+template <int FMT, bool POW2, bool F32, class F>
+__device__ __forceinline__ u32x2_t codes8(const float (&x)[8], float about, F &&divisor)
+{
+    float v[8];
+    auto all = [&](auto &&f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = f(x[j]);
+        return u32x2_t{pack4<FMT>(v[0], v[1], v[2], v[3]), pack4<FMT>(v[4], v[5], v[6], v[7])};
+    };
+    auto in_steps = [&] {
+        const Divisor d = divisor();
+        return all([&](float f) { return d.quotient<POW2, F32>(f); });
+    };
+    if constexpr (POW2 || !F32) return in_steps();
+    const float below = about * (1.0f - 0x1p-20f), above = about * (1.0f + 0x1p-20f);
+    const u32x2_t w = all([&](float f) { return f * below; }), u = all([&](float f) { return f * above; });
+    if ((w[0] ^ u[0]) | (w[1] ^ u[1])) return in_steps();
+    return w;
+}
 
 // A workgroup takes 32 rows x KT blocks of 128, 16 lanes to a block: a wave's load covers four blocks' 256 (bf16) bytes, and all of a
 // lane's 2 KT pieces are in flight before the first is used.  Scales of one block column and 32 rows leave together (128 bytes):
@@ -48,11 +113,11 @@ __global__ __launch_bounds__(kThreads) void quant_rows_kernel(QuantArgs a)
         uint32_t top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) { v[j] = piece_get(in[i], j); top = umax(top, mag_bits(v[j])); }
-        const BlockScale b = BlockScale::of<FMT, POW2>(row16_umax(top));
+        top = row16_umax(top);
+        const BlockScale b = BlockScale::of<FMT, POW2>(top);
+        const Divisor d = Divisor::of<FMT, POW2>(top, b);
         if (row0 + r < a.rows && kb < a.nkb) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = b.scaled<POW2>(v[j]);
-            const u32x2_t w = {pack4<FMT>(v[0], v[1], v[2], v[3]), pack4<FMT>(v[4], v[5], v[6], v[7])};
+            const u32x2_t w = codes8<FMT, POW2, sizeof(T) == 4>(v, d.about(), [&] { return d; });
             *reinterpret_cast<u32x2_t *>(a.Q + (int64_t)(row0 + r) * a.ldq + kb * 128 + p * 8) = w;
         }
         if (p == 0) scales[(item % KT) * 32 + r] = POW2 ? b.code : __float_as_uint(b.s);
@@ -96,15 +161,17 @@ __global__ __launch_bounds__(kThreads) void quant_tiles_kernel(QuantArgs a)
     top = wave_umax(top);
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
-    const BlockScale b = BlockScale::of<FMT, POW2>(umax(umax(tops[0], tops[1]), umax(tops[2], tops[3])));
+    top = umax(umax(tops[0], tops[1]), umax(tops[2], tops[3]));
+    const BlockScale b = BlockScale::of<FMT, POW2>(top);
+    const Divisor d = Divisor::of<FMT, POW2>(top, b);
     if (threadIdx.x == 0) store_scale<POW2>(a.S, (int64_t)kb * a.lds + rt, b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (r0 + 16 * i >= a.rows) break;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = b.scaled<POW2>(piece_get(in[i], j));
-        const u32x2_t w = {pack4<FMT>(v[0], v[1], v[2], v[3]), pack4<FMT>(v[4], v[5], v[6], v[7])};
+        for (int j = 0; j < 8; ++j) v[j] = piece_get(in[i], j);
+        const u32x2_t w = codes8<FMT, POW2, sizeof(T) == 4>(v, d.about(), [&] { return d; });
         *reinterpret_cast<u32x2_t *>(a.Q + (int64_t)(r0 + 16 * i) * a.ldq + col) = w;
     }
 }
@@ -116,7 +183,11 @@ template <class T, int FMT, bool POW2, bool TILE>
 __global__ __launch_bounds__(kThreads) void quant_turned_kernel(QuantArgs a)
 {
     __shared__ __align__(16) uint32_t maxima[TILE ? 4 : 16 * 128];
+    // of the columns, float32 scales: for float32 values the factor about right and the maximum, else the divisor in two parts; e8m0: the
+    // factor
+    constexpr bool F32 = sizeof(T) == 4 && !POW2;
     __shared__ __align__(16) uint2 factors[TILE ? 1 : 128];
+    __shared__ __align__(16) float pres[TILE || POW2 || F32 ? 1 : 128];
     __shared__ __align__(16) uint2 codes[128 * 16];
     const int ct = blockIdx.x % a.groups, kb = blockIdx.x / a.groups;
     const int cc = threadIdx.x & 15, rg = threadIdx.x >> 4;
@@ -127,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void quant_turned_kernel(QuantArgs a)
         in[i] = load8(static_cast<const T *>(a.X) + (int64_t)min(r0 + i, a.rows - 1) * a.ldx, col, a.c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) settle(in[i], r0 + i < a.rows ? a.c - col : 0, a.c);
-    BlockScale one{};
+    Divisor one{};
     if constexpr (TILE) {
         uint32_t top = 0;
 #pragma unroll
@@ -137,8 +208,10 @@ __global__ __launch_bounds__(kThreads) void quant_turned_kernel(QuantArgs a)
         top = wave_umax(top);
         if ((threadIdx.x & 63) == 0) maxima[threadIdx.x >> 6] = top;
         __syncthreads();
-        one = BlockScale::of<FMT, POW2>(umax(umax(maxima[0], maxima[1]), umax(maxima[2], maxima[3])));
-        if (threadIdx.x == 0) store_scale<POW2>(a.S, (int64_t)kb * a.lds + ct, one);
+        top = umax(umax(maxima[0], maxima[1]), umax(maxima[2], maxima[3]));
+        const BlockScale b = BlockScale::of<FMT, POW2>(top);
+        one = Divisor::of<FMT, POW2>(top, b);
+        if (threadIdx.x == 0) store_scale<POW2>(a.S, (int64_t)kb * a.lds + ct, b);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -153,7 +226,9 @@ __global__ __launch_bounds__(kThreads) void quant_turned_kernel(QuantArgs a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = umax(top, maxima[i * 128 + threadIdx.x]);
             const BlockScale b = BlockScale::of<FMT, POW2>(top);
-            factors[threadIdx.x] = make_uint2(__float_as_uint(b.rc), __float_as_uint(b.top2));
+            const Divisor d = Divisor::of<FMT, POW2>(top, b);
+            factors[threadIdx.x] = F32 ? make_uint2(__float_as_uint(d.about()), top) : make_uint2(__float_as_uint(d.rc), __float_as_uint(d.top2));
+            if constexpr (!POW2 && !F32) pres[threadIdx.x] = d.pre;
             const int n = ct * 128 + (int)threadIdx.x;
             if (n < a.c) store_scale<POW2>(a.S, (int64_t)kb * a.lds + n, b);
         }
@@ -161,16 +236,20 @@ __global__ __launch_bounds__(kThreads) void quant_turned_kernel(QuantArgs a)
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        BlockScale b = one;
-        if constexpr (!TILE) {
-            const uint2 f = factors[cc * 8 + j];
-            b.rc = __uint_as_float(f.x);
-            b.top2 = __uint_as_float(f.y);
-        }
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = b.scaled<POW2>(piece_get(in[i], j));
-        codes[(cc * 8 + j) * 16 + (rg ^ cc)] = make_uint2(pack4<FMT>(v[0], v[1], v[2], v[3]), pack4<FMT>(v[4], v[5], v[6], v[7]));
+        for (int i = 0; i < 8; ++i) v[i] = piece_get(in[i], j);
+        u32x2_t w;
+        if constexpr (TILE) {
+            w = codes8<FMT, POW2, F32>(v, one.about(), [&] { return one; });
+        } else {
+            const uint2 f = factors[cc * 8 + j];
+            w = codes8<FMT, POW2, F32>(v, __uint_as_float(f.x), [&] {
+                if constexpr (F32) return Divisor::of<FMT, false>(f.y, BlockScale{});
+                return Divisor{__uint_as_float(f.x), __uint_as_float(f.y), POW2 ? 0.0f : pres[cc * 8 + j]};
+            });
+        }
+        codes[(cc * 8 + j) * 16 + (rg ^ cc)] = make_uint2(w[0], w[1]);
     }
     __syncthreads();
 #pragma unroll

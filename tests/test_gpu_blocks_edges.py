@@ -156,3 +156,64 @@ def test_codes_of_more_rows_than_a_launch_takes():
     assert bool((S[:, :-200] == one.item()).all()) and bool((Q[:-200, 0].view(torch.uint8) == 0x7E).all())
     del X, Q, S
     torch.cuda.empty_cache()
+
+
+FORMATS = {"e4m3": (torch.float8_e4m3fn, 448.0), "e5m2": (torch.float8_e5m2, 57344.0)}
+
+
+def next_to_borders(fmt, top, dtype):
+    """[128, 128]: the values of one block (its rows', its columns', the tile's largest magnitude is top) that lie nearest to a border
+    between two codes, and the float32 values beside them."""
+    kind, most = FORMATS[fmt]
+    codes = torch.arange(0, 128 if fmt == "e4m3" else 124, dtype=torch.uint8).view(kind).float().double()
+    codes = codes[codes.isfinite()]
+    near = ((codes[1:] + codes[:-1]) / 2 * top / most).to(dtype)
+    if dtype == torch.float32:
+        near = torch.cat([near, torch.nextafter(near, torch.zeros(())), torch.nextafter(near, torch.full((), 3e38))])
+    v = near[torch.arange(128 * 128) % len(near)].reshape(128, 128)
+    v = torch.where(torch.arange(128 * 128).reshape(128, 128) % 5 < 2, -v, v)
+    v[0, :] = v[:, 0] = top
+    return v
+
+
+def codes_like_the_oracle(x, blocks, fmt, pow2):
+    rows, c = x.shape
+    r, k = (c, ref.up(rows)) if blocks in ("cols", "tiles_t") else (rows, ref.up(c))
+    n = -(-r // 128) if blocks.startswith("tiles") else r
+    Q = torch.full((r, k), 0x55, dtype=torch.uint8, device=dev()).view(FORMATS[fmt][0])
+    S = torch.empty(k // 128, n, dtype=torch.uint8 if pow2 else torch.float32, device=dev())
+    trdq.fp8_quant(x.to(dev()), Q, S, blocks=blocks)
+    torch.cuda.synchronize()
+    want, s, _ = ref.quant(x, blocks, fmt, pow2)
+    got = S.cpu().double() if not pow2 else torch.pow(2.0, S.cpu().double() - 127)
+    assert torch.equal(got, s.float().double()), (blocks, fmt, pow2)
+    bad = Q.cpu().float().double() != want
+    assert not bool(bad.any()), (blocks, fmt, pow2, int(bad.sum()))
+
+
+@pytest.mark.parametrize("blocks", ["rows", "cols", "tiles", "tiles_t"])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_codes_next_to_borders(blocks, fmt, dtype):
+    """Every code is the nearest to the exact quotient: float32 values within a rounding of a border, and bf16 ones on it (the largest
+    value is 7 times a power of two), in blocks from the smallest scale to the largest."""
+    g = torch.Generator().manual_seed(11)
+    tiles = []
+    for e in (-100, -99, -95, -90, -85, -80, -60, -20, 0, 3, 40, 100, 126, 127):
+        if dtype == torch.float32:
+            mantissa = 1.0 + torch.randint(0, 2 ** 23, (), generator=g).item() * 2.0 ** -23
+        else:
+            mantissa = 1.75
+        tiles.append(next_to_borders(fmt, mantissa * 2.0 ** e, dtype))
+    x = torch.cat(tiles, 1)
+    for pow2 in (False, True):
+        codes_like_the_oracle(x, blocks, fmt, pow2)
+
+
+@pytest.mark.parametrize("blocks", ["rows", "cols", "tiles", "tiles_t"])
+def test_codes_of_any_float32(blocks):
+    """Every code of ordinary float32 values, at a ragged size."""
+    x = rand(21, 1000, 1411) * torch.exp2(rand(22, 1000, 1411).mul(6).round())
+    for fmt in FORMATS:
+        for pow2 in (False, True):
+            codes_like_the_oracle(x, blocks, fmt, pow2)
