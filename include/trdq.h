@@ -538,10 +538,12 @@ trdq_status trdq_fp8_quant(const void *X_dev, int x_dtype, int64_t rows, int c, 
  * With a linear y = x W^T (W [out, in]): forward A = ROWS(x), B = TILES(W); input gradient A = ROWS(dy), B = TILES_T(W);
  * weight gradient A = COLS(dy), B = COLS(x).
  * ws_dev: at least trdq_fp8_gemm_ws_nbytes(M, N, K) bytes (0: may be NULL), 16-byte aligned, the call's own until it has
- * finished; nothing in it has to be kept or cleared.
+ * finished; nothing in it has to be kept or cleared.  That size is of these M, N, K alone (of fewer rows K may be split further, and more is
+ * needed); trdq_fp8_gemm_ws_nbytes_upto(M, N, K) bytes, at most 2^26, are enough for every product whose sizes are at most these.
  * M == 0 is a no-op.  Errors: NULL -> ERR_NULL; sizes, strides, alignment, a workspace that is too small -> ERR_SHAPE;
  * another type than listed, or M >= 2^31 - 256 -> ERR_UNSUPPORTED. */
 size_t trdq_fp8_gemm_ws_nbytes(int64_t M, int N, int K);
+size_t trdq_fp8_gemm_ws_nbytes_upto(int64_t M, int N, int K);
 trdq_status trdq_fp8_gemm(int64_t M, int N, int K, const void *A_dev, int a_dtype, int64_t lda, const void *sa_dev, int64_t ldsa,
                           const void *B_dev, int b_dtype, int64_t ldb, const void *sb_dev, int64_t ldsb, int b_tiles, int s_dtype,
                           const float *bias_dev, void *Y_dev, int y_dtype, int64_t ldy, void *ws_dev, size_t ws_bytes,
@@ -589,7 +591,8 @@ trdq_status trdq_block_norm(const trdq_norm *n, const void *X_dev, int64_t ldx, 
  * may be Y): what leaves.  Statistics are computed again.  Gradients of parameters, float32 and dense: dscale, dshift [segments, c], dgate
  * [segments, c], or [c] of a gate with ld_gate == 0, the others [c]; each may be NULL, and is if its parameter is.  Written, not added to; sums over rows run in a
  * fixed order.  ws_dev: trdq_block_norm_bwd_ws_nbytes(rows, c, segments) bytes, 16-byte aligned, the call's own until it has
- * finished (may be NULL if no parameter's gradient is asked for).  rows == 0: the gradients asked for become zeros, nothing else
+ * finished (may be NULL if no parameter's gradient is asked for); of fewer rows or segments it may be larger, but never more than
+ * 16 c (512 + segments).  rows == 0: the gradients asked for become zeros, nothing else
  * is read or written (dscale, dshift and a dgate by segment have no rows then with seg_len > 0, n_seg rows with seg_off).
  * Errors as trdq_block_norm; a parameter's gradient without the parameter -> ERR_NULL; Y without dY or dY without Y, a workspace that
  * is too small -> ERR_SHAPE. */

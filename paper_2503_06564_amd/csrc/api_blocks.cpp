@@ -101,6 +101,12 @@ size_t trdq_fp8_gemm_ws_nbytes(int64_t M, int N, int K)
     return trdq::fp8_gemm_workspace_bytes(M, N, K);
 }
 
+size_t trdq_fp8_gemm_ws_nbytes_upto(int64_t M, int N, int K)
+{
+    if (M <= 0 || M >= kMostRows || N <= 0 || K <= 0) return 0;
+    return trdq::fp8_gemm_workspace_bytes_upto(M, N, K);
+}
+
 trdq_status trdq_fp8_gemm(int64_t M, int N, int K, const void *A_dev, int a_dtype, int64_t lda, const void *sa_dev, int64_t ldsa,
                           const void *B_dev, int b_dtype, int64_t ldb, const void *sb_dev, int64_t ldsb, int b_tiles, int s_dtype,
                           const float *bias_dev, void *Y_dev, int y_dtype, int64_t ldy, void *ws_dev, size_t ws_bytes, void *stream)

@@ -601,6 +601,10 @@ constexpr DirectForm kDirectForms[] = {{kDirect11, 1, 1, 0.11f, 0.12f, 0.1f},   
                                        {kDirect22, 2, 2, 0.24f, 0.25f, 0.3f},      {kDirect22Long, 2, 2, 0.24f, 0.24f, 1.2f},
                                        {kDirect24, 2, 4, 0.37f, 0.42f, 0.3f}};
 
+constexpr int kSplits[] = {2, 3, 4, 6, 8};
+constexpr int kLeastBlocks = 4;              // of K, of a part
+constexpr int kMostParts = 1024, kMostLastParts = 320;
+
 Plan plan_of(int64_t M, int64_t N, int nkb, bool exact)
 {
     // up to 16 rows: one tile of 16 columns a workgroup (1 x 8192 x 8192 15.4 us, a copy's rate; two tiles 19.2), eight waves where K is
@@ -617,19 +621,23 @@ Plan plan_of(int64_t M, int64_t N, int nkb, bool exact)
         take(d.form, 1, 3.0f + (float)over(groups, 256) * ((float)nkb * (exact ? d.block_exact : d.block) + d.group));
     }
     const int64_t tiles = over(M, 128) * over(N, 128);
-    for (int splits : {1, 2, 3, 4, 6, 8}) {
-        if (splits > 1 && (nkb < 4 * splits || tiles * splits > 1024)) break;
+    auto tiled = [&](int splits) {
         const int64_t n = tiles * splits;
         const float block = n <= 256 ? (exact ? 1.15f : 0.63f) : (exact ? 2.0f : 0.85f) * (float)over(n, 512);
         take(kTile128, splits, 4.0f + block * (float)over(nkb, splits) + (splits == 1 ? out : 3.0f + (float)splits * (float)M * (float)N * 8.0f / 4.5e6f));
+    };
+    tiled(1);
+    for (int splits : kSplits) {
+        if (nkb < kLeastBlocks * splits || tiles * splits > kMostParts) break;
+        tiled(splits);
     }
     // more tiles than compute units: the last, incomplete round in parts (4 and 2 us for the second kernel and for what the estimate misses)
     const int64_t whole = tiles / 256 * 256, left = tiles - whole;
     if (whole > 0 && left > 0 && tiles <= 4096)
-        for (int splits : {2, 3, 4, 6, 8}) {
-            if (nkb < 4 * splits || left * splits > 320) break;
+        for (int splits : kSplits) {
+            if (nkb < kLeastBlocks * splits || left * splits > kMostLastParts) break;
             const float pair = exact ? 1.95f : 0.85f, alone = exact ? 1.15f : 0.63f;
-            const float tail = (float)over(nkb, splits) * (float)over(left * splits, 320), all = (float)(whole / 256) * (float)nkb;
+            const float tail = (float)over(nkb, splits) * (float)over(left * splits, kMostLastParts), all = (float)(whole / 256) * (float)nkb;
             take(kTile128, splits, 10.0f + (whole == 256 ? tail * pair + (all - tail) * alone : (all + tail) * 0.5f * pair) + out +
                                        (float)(left * splits) * 131072.0f / 4.5e6f, whole);
         }
@@ -682,6 +690,17 @@ size_t fp8_gemm_workspace_bytes(int64_t M, int N, int K)
         if (p.splits > 1) most = std::max(most, (size_t)(tiles - p.whole) * p.splits * 128 * 128 * sizeof(float));
     }
     return most;
+}
+
+// Enough for every smaller product too, whichever form its estimates take: at most kMostParts parts of tiles, and no more parts of a tile
+// than its K allows (the last rounds in parts, of fewer than 256 tiles behind whole ones, stay below that).
+size_t fp8_gemm_workspace_bytes_upto(int64_t M, int N, int K)
+{
+    const int64_t tiles = ((M + 127) / 128) * (int64_t)((N + 127) / 128);
+    int64_t most = 0;
+    for (int splits : kSplits)
+        if (K / 128 >= kLeastBlocks * splits) most = std::max(most, splits * std::min<int64_t>(tiles, kMostParts / splits));
+    return (size_t)most * 128 * 128 * sizeof(float);
 }
 
 template <bool EXACT>

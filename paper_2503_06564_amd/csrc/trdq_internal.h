@@ -211,6 +211,7 @@ struct Fp8GemmArgs {
     bool out_f32, b_tiles;
 };
 size_t fp8_gemm_workspace_bytes(int64_t M, int N, int K);
+size_t fp8_gemm_workspace_bytes_upto(int64_t M, int N, int K);
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &a, bool a_e5m2, bool pow2, bool b_tiles, hipStream_t st);
 
 }  // namespace trdq

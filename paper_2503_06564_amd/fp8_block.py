@@ -29,7 +29,8 @@ def _codes(rows, k, fmt, device, tiles=False):
 
 
 class Fp8Linear:
-    """y = x W^T + b with W [out, in] float32, products of codes.  `tokens` is the most rows of x; every buffer is made here."""
+    """y = x W^T + b with W [out, in] float32, products of codes.  `tokens` is the most rows of x (fewer, or none, use the front of the
+    buffers, all of which are made here)."""
 
     def __init__(self, W, b, tokens):
         import torch
@@ -39,8 +40,8 @@ class Fp8Linear:
         self.w, self.wt = _codes(out, inn, "e4m3", dev, tiles=True), _codes(inn, out, "e4m3", dev, tiles=True)
         self.xt, self.dy, self.dyt = _codes(inn, tokens, "e4m3", dev), _codes(tokens, out, "e5m2", dev), _codes(out, tokens, "e5m2", dev)
         self.dW, self.db = torch.empty_like(W), torch.empty_like(b)
-        need = max(trdq.fp8_gemm_ws_nbytes(tokens, out, _up(inn)), trdq.fp8_gemm_ws_nbytes(tokens, inn, _up(out)),
-                   trdq.fp8_gemm_ws_nbytes(out, inn, _up(tokens)))
+        need = max(trdq.fp8_gemm_ws_nbytes_upto(tokens, out, _up(inn)), trdq.fp8_gemm_ws_nbytes_upto(tokens, inn, _up(out)),
+                   trdq.fp8_gemm_ws_nbytes_upto(out, inn, _up(tokens)))
         self.ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
         self.ones = torch.ones(1, tokens, device=dev)
         self.set_weights()
@@ -56,12 +57,20 @@ class Fp8Linear:
     def backward(self, x, dy, dx):
         """dx (bf16), dW and db from dy (bf16) and the input x (bf16)."""
         import torch
-        trdq.fp8_quant(dy, *self.dy, blocks="rows")
-        trdq.fp8_gemm(*self.dy, *self.wt, dx, ws=self.ws)
-        trdq.fp8_quant(dy, *self.dyt, blocks="cols")
-        trdq.fp8_quant(x, *self.xt, blocks="cols")
-        trdq.fp8_gemm(*self.dyt, *self.xt, self.dW, ws=self.ws)
-        torch.matmul(self.ones, dy.float(), out=self.db[None])      # (a sum over rows would clear memory in a captured graph)
+        rows = x.shape[0]
+        if rows == 0:                                               # (a product has a block of K at least)
+            self.dW.zero_()
+            self.db.zero_()
+            return
+        by_rows = lambda c: (c[0][:rows], c[1][:, :rows])  # noqa: E731
+        by_cols = lambda c: (c[0][:, :_up(rows)], c[1][:_up(rows) // trdq.BLOCK])  # noqa: E731
+        dyq, dyt, xt = by_rows(self.dy), by_cols(self.dyt), by_cols(self.xt)
+        trdq.fp8_quant(dy, *dyq, blocks="rows")
+        trdq.fp8_gemm(*dyq, *self.wt, dx, ws=self.ws)
+        trdq.fp8_quant(dy, *dyt, blocks="cols")
+        trdq.fp8_quant(x, *xt, blocks="cols")
+        trdq.fp8_gemm(*dyt, *xt, self.dW, ws=self.ws)
+        torch.matmul(self.ones[:, :rows], dy.float(), out=self.db[None])      # (a sum over rows would clear memory in a captured graph)
 
 
 class MlpBlock:

@@ -33,7 +33,7 @@ SYMBOLS = [
     "trdq_xq_tiled_nbytes", "trdq_rotate_quant_tiled", "trdq_xq_untile", "trdq_qgemm_tiled_supported", "trdq_qgemm_tiled_preferred",
     "trdq_qgemm_tiled",
     "trdq_rotate_quant_rpr_asym", "trdq_prepare_weights_asym", "trdq_weights_export_zero_points", "trdq_qgemm_asym_weights",
-    "trdq_fp8_quant", "trdq_fp8_gemm", "trdq_fp8_gemm_ws_nbytes",
+    "trdq_fp8_quant", "trdq_fp8_gemm", "trdq_fp8_gemm_ws_nbytes", "trdq_fp8_gemm_ws_nbytes_upto",
     "trdq_block_norm", "trdq_block_norm_bwd", "trdq_block_norm_bwd_ws_nbytes",
 ]
 
@@ -146,8 +146,9 @@ def lib():
         L.trdq_qgemm_num_variants.restype = i32
         sz = C.c_size_t
         L.trdq_fp8_quant.argtypes = [p, i32, i64, i32, i64, i32, i32, p, i64, i32, p, i64, p]
-        L.trdq_fp8_gemm_ws_nbytes.argtypes = [i64, i32, i32]
-        L.trdq_fp8_gemm_ws_nbytes.restype = sz
+        for f in (L.trdq_fp8_gemm_ws_nbytes, L.trdq_fp8_gemm_ws_nbytes_upto):
+            f.argtypes = [i64, i32, i32]
+            f.restype = sz
         L.trdq_fp8_gemm.argtypes = [i64, i32, i32, p, i32, i64, p, i64, p, i32, i64, p, i64, i32, i32, p, p, i32, i64, p, sz, p]
         L.trdq_block_norm.argtypes = [p, p, i64, p, i64, p, i64, i32, p, i64, i32, p, i64, p]
         L.trdq_block_norm_bwd_ws_nbytes.argtypes = [i64, i32, i64]
@@ -788,7 +789,13 @@ def fp8_quant(X, Q, S, blocks="rows", stream=None):
 
 
 def fp8_gemm_ws_nbytes(M, N, K):
+    """Workspace bytes of a product of these sizes (K: of the codes); one of fewer rows may need more."""
     return lib().trdq_fp8_gemm_ws_nbytes(M, N, K)
+
+
+def fp8_gemm_ws_nbytes_upto(M, N, K):
+    """Enough for every product of at most these sizes."""
+    return lib().trdq_fp8_gemm_ws_nbytes_upto(M, N, K)
 
 
 def fp8_gemm(A, sa, B, sb, Y, bias=None, ws=None, stream=None):

@@ -123,3 +123,23 @@ def test_most_rows():
             norm.rows = rows
             assert call(rows) == want, (name, rows)
     assert trdq.block_norm_bwd_ws_nbytes(2 ** 31 - 257, 40, 1) > 0
+
+
+def test_one_workspace_for_smaller_products():
+    """Fewer rows may need a larger workspace (K is split further): one that is made for the largest sizes has a query of its own."""
+    own, upto = trdq.fp8_gemm_ws_nbytes, trdq.fp8_gemm_ws_nbytes_upto
+    assert any(own(m, 1152, 4608) > own(4096, 1152, 4608) for m in range(1, 4096))
+    g = torch.Generator().manual_seed(1)
+    draw = lambda n: int(torch.exp(torch.rand((), generator=g) * torch.log(torch.tensor(float(n)))))  # noqa: E731
+    for M, N, K in ((4096, 1152, 4608), (8192, 4608, 1152), (4608, 1152, 8192), (300, 500, 640), (17, 64, 16384), (2100, 2200, 4224), (32768, 8192, 8192),
+                    (2 ** 31 - 257, 128, 128)):
+        most = upto(M, N, K)
+        assert own(M, N, K) <= most <= 64 << 20
+        for _ in range(400):
+            m, n, k = draw(M), draw(N), -(-draw(K) // 128) * 128
+            assert own(m, n, k) <= most and own(m, N, K) <= most and upto(m, n, k) <= most, (m, n, k)
+        for m in range(1, min(M, 3000), 7):
+            assert own(m, N, K) <= most, m
+    assert upto(0, 128, 1024) == 0 and upto(128, 0, 1024) == 0 and upto(128, 128, 0) == 0 and upto(128, 128, 896) == 0
+    for bad in ((2 ** 31, 128, 1024), (-1, 128, 1024)):
+        assert upto(*bad) == 0
