@@ -1,5 +1,6 @@
 """Compile libtrdq.so (HIP kernels + C ABI) for gfx950 with hipcc, in-tree."""
 import os
+import shutil
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -44,13 +45,38 @@ def _compile(src, extra, obj_dir):
     return obj, out
 
 
-def build_calls(out=CALLS):
-    """The Python module block_calls.cpp: host code only, linked to libtrdq.so beside it and to the installed torch."""
+def _calls_headers():
+    """Where the headers of torch and Python lie."""
     import sysconfig
 
-    import torch
     from torch.utils import cpp_extension
-    inc = [f"-isystem{p}" for p in cpp_extension.include_paths("cuda")] + [f"-isystem{sysconfig.get_paths()['include']}"]
+    return [*cpp_extension.include_paths("cuda"), sysconfig.get_paths()["include"]]
+
+
+def _calls_lack():
+    """What block_calls.cpp needs beside its source and is not here, or None."""
+    if shutil.which("g++") is None:
+        return "g++"
+    try:
+        dirs = _calls_headers()
+    except ImportError as e:
+        return str(e)
+    return next((h for h in ("Python.h", "torch/csrc/autograd/python_variable.h", "c10/hip/HIPStream.h")
+                 if not any(os.path.exists(os.path.join(d, h)) for d in dirs)), None)
+
+
+def build_calls(out=CALLS):
+    """The Python module block_calls.cpp: host code only, linked to libtrdq.so beside it and to the installed torch.  Where its compiler or
+    headers are missing, none is built (the C library and the rest of the binding need neither): says so, and returns None.  The
+    calls that need it raise then; a module of an earlier build is never left behind."""
+    if os.path.exists(out):
+        os.remove(out)
+    lack = _calls_lack()
+    if lack:
+        print(f"{os.path.basename(out)} is not built, its calls will raise: {lack} is missing", file=sys.stderr)
+        return None
+    import torch
+    inc = [f"-isystem{p}" for p in _calls_headers()]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, *inc, os.path.join(CSRC, "block_calls.cpp"), "-o", out,
