@@ -217,3 +217,33 @@ def test_codes_of_any_float32(blocks):
     for fmt in FORMATS:
         for pow2 in (False, True):
             codes_like_the_oracle(x, blocks, fmt, pow2)
+
+
+@pytest.mark.parametrize("m,k,n", [(16, 8192, 512), (100, 4096, 300), (512, 1152, 3456), (1000, 8192, 1152), (2100, 4100, 2200)])
+@pytest.mark.parametrize("a_fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("hot", [False, True])
+def test_products_as_a_whole(m, k, n, a_fmt, pow2, hot):
+    """The norm of a product's error beside the norm of the product.  Outputs in bf16: rounding is even over half a step, at most 2^-8 / sqrt 3 =
+    2.26e-3.  The instruction cuts seven of eight products by up to 2^-13 of the largest, which is three to four times their root mean
+    square: sqrt(7 / 3 / 8) 2^-13 4 = 2.6e-4 without a common sign, the two together 2.27e-3 (a common sign would add up over K: 2e-2 at
+    8192).  Outputs in float32: 16 roundings in a block and one a block, of sums no larger than the last on the whole,
+    sqrt(16 + 64) 2^-24 = 5.3e-7 and twice that for sums cut in place of rounded."""
+    x, w = rand(31, m, k), rand(32, n, k) * 0.02
+    if hot:
+        x[:, ::128] *= 20.0
+    qa, sa, _ = ref.quant(x.to(torch.bfloat16), "rows", a_fmt, pow2)
+    qb, sb, _ = ref.quant(w, "tiles", "e4m3", pow2)
+    A, B = qa.float().to(dev()).to(FORMATS[a_fmt][0]), qb.float().to(dev()).to(FORMATS["e4m3"][0])
+    put = lambda s: torch.log2(s).add(127).to(torch.uint8).to(dev()) if pow2 else s.to(dev())  # noqa: E731
+    sa, sb = sa.float(), sb.float()
+    need = trdq.fp8_gemm_ws_nbytes(m, n, A.shape[1])
+    ws = torch.empty(need, dtype=torch.uint8, device=dev()) if need else None
+    want = (qa * ref.wide(sa, *qa.shape)).to(dev()) @ (qb * ref.wide(sb, *qb.shape)).to(dev()).t()
+    for dtype, bound in ((torch.bfloat16, 2.3e-3), (torch.float32, 1.1e-6)):
+        Y = torch.empty(m, n, dtype=dtype, device=dev())
+        trdq.fp8_gemm(A, put(sa), B, put(sb), Y, ws=ws)
+        torch.cuda.synchronize()
+        err = float((Y.double() - want).norm() / want.norm())
+        print(f"{m} x {k} x {n} {a_fmt} pow2={pow2} hot={hot} {dtype}: {err:.3e}", flush=True)
+        assert err <= bound, (dtype, err)
