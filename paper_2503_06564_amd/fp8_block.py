@@ -132,6 +132,8 @@ class MlpBlock:
 
 def train(tokens, width, batch, steps, rate=2.0, seed=0):
     """Losses of `steps` steps towards a fixed random target, and the seconds of one."""
+    if steps < 1:
+        raise ValueError("steps: one at least")
     import torch
     g = torch.Generator().manual_seed(seed + 1)
     x, y, target = ((torch.randn(tokens, width, generator=g)).to("cuda").to(torch.bfloat16) for _ in range(3))

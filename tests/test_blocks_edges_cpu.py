@@ -143,3 +143,10 @@ def test_one_workspace_for_smaller_products():
     assert upto(0, 128, 1024) == 0 and upto(128, 0, 1024) == 0 and upto(128, 128, 0) == 0 and upto(128, 128, 896) == 0
     for bad in ((2 ** 31, 128, 1024), (-1, 128, 1024)):
         assert upto(*bad) == 0
+
+
+def test_training_takes_a_step_at_least():
+    from paper_2503_06564_amd import fp8_block
+    for steps in (0, -1):
+        with pytest.raises(ValueError, match="steps"):
+            fp8_block.train(128, 128, 1, steps)
