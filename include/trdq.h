@@ -517,7 +517,8 @@ typedef enum trdq_dtype {
  *   TRDQ_BLOCKS_TILES    [rows, up(c)]         [up(c) / 128, ceil(rows / 128)]           128 x 128 tiles
  *   TRDQ_BLOCKS_TILES_T  [c, up(rows)]         [up(rows) / 128, ceil(c / 128)]           the same, codes transposed
  * with up(k) = k rounded up to 128; codes behind the end of a row are zeros.  ldq: row stride of Q (>= up(k), a multiple of
- * 16; Q 16-byte aligned); lds: row stride of S in scales.  A block that holds Inf or NaN gets a NaN as its scale and codes.
+ * 16; Q 16-byte aligned); lds: row stride of S in scales.  A block that holds Inf or NaN gets a NaN as its scale and codes (those behind
+ * the end of its rows too).
  * rows == 0 is a no-op.
  * Errors: NULL X/Q/S -> ERR_NULL; rows < 0, c <= 0, strides, alignment -> ERR_SHAPE; unknown blocks -> ERR_RANGE; another
  * type than listed, rows >= 2^31 - 256 or c > 2^24 -> ERR_UNSUPPORTED. */
@@ -532,7 +533,8 @@ trdq_status trdq_fp8_quant(const void *X_dev, int x_dtype, int64_t rows, int c, 
  * A [M, K] in e4m3 or e5m2 with sa [K / 128, M]; B [N, K] in e4m3 with sb [K / 128, N], or with b_tiles != 0
  * [K / 128, ceil(N / 128)].  K % 128 == 0 (codes as trdq_fp8_quant pads them); lda, ldb multiples of 16 and at most 2^22, bases
  * 16-byte aligned; ldsa, ldsb: row strides of the scales (their type is the same for both).  bias float32 [N] or NULL; Y
- * bf16 or float32 with row stride ldy >= N.  Float32 outputs: products are exact, sums and scales float32.  bf16 outputs: the
+ * bf16 or float32 with row stride ldy >= N.  Float32 outputs: products are exact, sums and scales float32 (sa sb too, formed before it meets a
+ * sum: it has to be a float32 number).  bf16 outputs: the
  * matrix instruction for 8-bit codes adds each eight neighbouring products after shifting them to the largest (13 bits below its
  * leading one are kept), every other sum is float32, one rounding at the end.
  * With a linear y = x W^T (W [out, in]): forward A = ROWS(x), B = TILES(W); input gradient A = ROWS(dy), B = TILES_T(W);
@@ -557,7 +559,8 @@ trdq_status trdq_fp8_gemm(int64_t M, int N, int K, const void *A_dev, int a_dtyp
  * (weight 1, bias 0, scale 0, shift 0, gate 1).  scale, shift and gate are [segments, c] with row strides ld_*; a gate with ld_gate
  * == 0 is one vector for every row.  A row's segment: row / seg_len if seg_len > 0; else, if seg_off is given (int32
  * [n_seg + 1] on the device, not decreasing), the one whose rows [seg_off[s], seg_off[s + 1]) it is in (rows before the first or
- * behind the last border belong to the first and last segment); else there is one.  Segments may be empty. */
+ * behind the last border belong to the first and last segment); else there is one.  Segments may be empty: no output depends on their
+ * parameters.  Statistics are float32: values whose squares leave its range (about 1e-19 and less beside eps = 0, 1e19 and more) have no norm. */
 typedef enum trdq_norm_kind { TRDQ_NORM_NONE = 0, TRDQ_NORM_LAYER = 1, TRDQ_NORM_RMS = 2 } trdq_norm_kind;
 typedef struct trdq_norm {
     int64_t rows;

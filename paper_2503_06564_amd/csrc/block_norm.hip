@@ -294,7 +294,9 @@ __global__ __launch_bounds__(Forward<W>::kThreads) void block_norm_kernel(NormAr
 // Slot of workgroup g's sums of segment s: g + s.  Neither ever decreases along the rows, so no two pairs meet, and a segment's
 // slots lie together.
 // All of a row's loads go out before its first reduction.  The factors (1 + scale) w and gate w2 are formed once a segment and wait in
-// shared memory: in registers, beside the sums and a row, they spill.
+// shared memory: in registers, beside the sums and a row, they spill.  What spills still: at three pieces a lane (1025 to 1536 values)
+// up to 46 registers with all four sums, up to 10 with three; at 16 waves (above 8192 values, 128 registers a lane) 35 to 178, in every
+// form: 4096 rows of 8192 bf16 values take 104 us, of 8704 567, of 16384 635.
 constexpr int kBwdWaves = 8;                          // of a workgroup whose waves have a row each
 template <int W, int NCH>
 constexpr size_t bwd_factor_bytes() { return 2 * (size_t)(64 * W) * NCH * 8 * sizeof(float); }
@@ -617,8 +619,8 @@ __global__ __launch_bounds__(256) void block_norm_zero_kernel(ZeroArgs a)
 }
 
 // Waves of a row and pieces of a lane.  Up to 1024 values one wave.  Up to 1536 the gradient keeps one wave (three waves a row, each with its
-// sums to write: 4096 x 1152 26 us in place of 21); forward three waves with one piece a lane take 57 registers in place of 147, eight
-// waves a SIMD in place of three (us, one wave / three: 4096 x 1152 bf16 13.3 / 11.8, float32 to codes 32768 x 1152 98.1 / 98.2, one
+// sums to write: 4096 x 1152 26 us in place of 21); forward three waves with one piece a lane take 43 to 49 registers in place of 94 to 147, eight
+// waves a SIMD in place of three to five (us, one wave / three: 4096 x 1152 bf16 13.3 / 11.8, float32 to codes 32768 x 1152 98.1 / 98.2, one
 // row 3.0 / 2.6).  Wider rows: a workgroup each.
 template <bool FORWARD, class F>
 hipError_t by_width(int c, F &&f)

@@ -6,7 +6,7 @@
 // the result off, with one value in 128 twenty times larger 3.2e-5: far below the 2^-4 that a code itself is off and the 2^-8 of
 // an output in bf16, but not an error that a float32 output should have.  So outputs in bf16 take this instruction, and
 // outputs in float32 (gradients of weights, which are summed further) widen the codes to bf16, exactly, and take the bf16
-// instruction, whose sums are float32 throughout (1.5e-8) at half the rate.
+// instruction, whose sums are float32 throughout (errors 4e-8 of the product's norm at K = 1152, 1.04e-7 at 8192) at half the rate.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
